@@ -42,6 +42,9 @@ __device__ __forceinline__ float bounded_abs(float x) {
   return r;
 }
 constexpr float kLog2e = 1.4426950409f;
+// x^2 in the derivative of tanh GELU's argument, which meets f (1 - p) = 0 far out: x^2 is infinite from
+// 1.8e19 on, and its product with 0 would be NaN (a NaN x reaches the result by f)
+constexpr float kSquareMax = 1e30f;
 constexpr float kHalfLog2eLow = -9.62981495e-09f;   // -1 / (2 ln 2) less its FP32 rounding
 __device__ constexpr float kExp2[6] = {0.693147182f, 0.240226477f, 0.0555033237f, 0.00961843692f, 0.0013398875f, 0.00015353359f};
 __device__ constexpr float kTail[9] = {0.139621302485466f,  0.13986355066299438f, 0.11982102692127228f,
@@ -90,7 +93,7 @@ __device__ __forceinline__ void activation_full(float x, float& f, float& df) {
     if constexpr (kAct == SQ_ACT_GELU_TANH) {
       const float x2 = x * x;
       z = x * fmaf(0.0713548163f, x2, 1.5957691216f);
-      dz = fmaf(0.2140644488f, x2, 1.5957691216f);
+      dz = fmaf(0.2140644488f, fminf(x2, kSquareMax), 1.5957691216f);
     }
     const float p = 1.0f / (1.0f + expf(-z));
     f = x * p;
@@ -131,7 +134,8 @@ __device__ __forceinline__ void activation_pair(float2 x, float2& f, float2& df)
       const float2 x2 = mul2(x, x);
       const float a = 1.5957691216f, b = 0.0713548163f;
       z = mul2(x, fma2(x2, make_float2(-b * kLog2e, -b * kLog2e), make_float2(-a * kLog2e, -a * kLog2e)));
-      if constexpr (kDeriv) dz = fma2(x2, make_float2(3.0f * b, 3.0f * b), make_float2(a, a));
+      if constexpr (kDeriv)
+        dz = fma2(make_float2(fminf(x2.x, kSquareMax), fminf(x2.y, kSquareMax)), make_float2(3.0f * b, 3.0f * b), make_float2(a, a));
     } else {
       z = mul2(x, make_float2(-kLog2e, -kLog2e));
     }
