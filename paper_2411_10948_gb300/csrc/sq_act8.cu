@@ -267,10 +267,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) act8_backward_ker
     if (r >= a.R) return;
     b.dy.load(dy + r * a.ld_in, c, a.C, true, lane);
     b.qa = ld_codes8(codes + r * a.ld_codes);
-    b.sa = static_cast<uint32_t>(ld_here(scales + r * a.ld_scales));
+    b.sa = ld_scale(scales + r * a.ld_scales);
     if constexpr (kGated) {
       b.qu = ld_codes8(codes + r * a.ld_codes + cp);
-      b.su = static_cast<uint32_t>(ld_here(scales + r * a.ld_scales + blocks));
+      b.su = ld_scale(scales + r * a.ld_scales + blocks);
     }
   };
   int64_t r = static_cast<int64_t>(blockIdx.y) * blockDim.y + threadIdx.y;
@@ -282,8 +282,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) act8_backward_ker
       if (r >= a.R) break;
       float g[8], x[8], u[8], f[8], df[8], da[8], du[8];
       n[k].dy.values(g, buf, lane);
-      decode8(n[k].qa, scale_value(n[k].sa), x);
-      if constexpr (kGated) decode8(n[k].qu, scale_value(n[k].su), u);
+      decode8(n[k].qa, n[k].sa, x);
+      if constexpr (kGated) decode8(n[k].qu, n[k].su, u);
       fetch(n[k], r + kActRows * step);
       activation8<T, kAct, true>(x, f, df);
 #pragma unroll

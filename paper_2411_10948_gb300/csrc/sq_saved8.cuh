@@ -6,6 +6,8 @@
 
 namespace sq {
 
+constexpr uint32_t kScaleTop8 = 249;   // 2^122: from here on 127 2^e is beyond FP32
+
 // x 2^-e rounded to nearest even as bytes: adding 1.5 2^23 leaves the integer in the low bits
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
   const float2 i2 = make_float2(inv, inv), shift = make_float2(12582912.0f, 12582912.0f);
@@ -30,13 +32,21 @@ __device__ __forceinline__ void decode8(uint2 w, float2 (&q)[4]) {
   q[2] = add2(make_float2(f(y, 0x7540), f(y, 0x7541)), off);
   q[3] = add2(make_float2(f(y, 0x7542), f(y, 0x7543)), off);
 }
-__device__ __forceinline__ void decode8(uint2 w, float s, float (&f)[8]) {
+// The values of eight codes under a scale byte.  The largest numbers of a type with FP32's range keep as
+// 64 2^122, which FP32 does not hold: its largest number stands for them (an infinity would
+// make a derivative NaN that is 0 or 1).  A NaN stays.
+__device__ __forceinline__ void decode8(uint2 w, uint32_t scale, float (&f)[8]) {
+  const float s = scale_value(scale);
   float2 q[4];
   decode8(w, q);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     q[i] = mul2(q[i], make_float2(s, s));
     f[2 * i] = q[i].x, f[2 * i + 1] = q[i].y;
+  }
+  if (scale >= kScaleTop8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm("min.NaN.xorsign.abs.f32 %0, %0, 0f7F7FFFFF;" : "+f"(f[i]));
   }
 }
 
@@ -52,9 +62,7 @@ __device__ __forceinline__ uint2 ld_codes8(const int8_t* p) {
   asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
   return v;
 }
-__device__ __forceinline__ float ld_scale(const uint8_t* p) {
-  return scale_value(static_cast<uint32_t>(ld_here(p)));
-}
+__device__ __forceinline__ uint32_t ld_scale(const uint8_t* p) { return static_cast<uint32_t>(ld_here(p)); }
 
 // Eight elements of a row on their way: aligned rows as they lie, others as a warp's dense loads.
 template <typename T, bool kVec>
