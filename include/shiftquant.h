@@ -669,9 +669,9 @@ sq_status shiftquant_mx4_linear(const void *x, int dtype, int64_t M, int64_t K, 
 /* Activation functions and normalizations whose input is kept in 8 bits for the backward pass
  * (activation checkpoints; the paper has no counterpart).  A kept tensor is int8 codes q with a
  * power-of-two scale per 32 elements of a row: x~ = q 2^e, |q| <= 127, e the smallest with
- * max|x| <= 127 2^e (e >= -127), stored as the byte e + 127; q = x 2^-e to nearest even (where
- * q 2^e is 2^128, x~ is FP32's largest number).  A block
- * that holds a NaN or an infinity gets the byte 255 (its x~ are NaN) and sets SQ_DEV_NONFINITE.
+ * max|x| <= 127 2^e (e >= -127), stored as the byte e + 127; q = x 2^-e to nearest even (at
+ * e = 122, x~ is q 2^e less 2^-24 of it, so that FP32 holds it).  A block that holds a NaN or an
+ * infinity gets the byte 255 (its x~ are NaN) and sets SQ_DEV_NONFINITE.
  *   codes [rows, ld_codes]: 16-byte aligned, ld_codes a multiple of 16, a row padded to whole
  *     blocks: 32 ceil(cols / 32) bytes.  scales [rows, ld_scales]: ceil(cols / 32) bytes a row.
  * Arithmetic is FP32 (a row whose squares it does not hold, from 1.8e19 on, has reciprocal

@@ -6,7 +6,7 @@
 
 namespace sq {
 
-constexpr uint32_t kScaleTop8 = 249;   // 2^122: from here on 127 2^e is beyond FP32
+constexpr uint32_t kScaleTop8 = 249;   // 2^122, the largest a finite block has
 
 // x 2^-e rounded to nearest even as bytes: adding 1.5 2^23 leaves the integer in the low bits
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
@@ -32,21 +32,21 @@ __device__ __forceinline__ void decode8(uint2 w, float2 (&q)[4]) {
   q[2] = add2(make_float2(f(y, 0x7540), f(y, 0x7541)), off);
   q[3] = add2(make_float2(f(y, 0x7542), f(y, 0x7543)), off);
 }
-// The values of eight codes under a scale byte.  The largest numbers of a type with FP32's range keep as
-// 64 2^122, which FP32 does not hold: its largest number stands for them (an infinity would
-// make a derivative NaN that is 0 or 1).  A NaN stays.
+// The value of a kept block's scale byte.  The largest numbers of a type with FP32's range keep as 64 2^122,
+// which FP32 does not hold: 2^122 less 2^-24 of it makes that FP32's largest number (an infinity would
+// make a derivative NaN that is 0 or 1).
+__device__ __forceinline__ float scale_value8(uint32_t byte) {
+  if (byte == kScaleNan) return __uint_as_float(0x7FC00000u);
+  return __uint_as_float(byte == 0 ? 0x00400000u : (byte << 23) - (byte == kScaleTop8 ? 1u : 0u));
+}
 __device__ __forceinline__ void decode8(uint2 w, uint32_t scale, float (&f)[8]) {
-  const float s = scale_value(scale);
+  const float s = scale_value8(scale);
   float2 q[4];
   decode8(w, q);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     q[i] = mul2(q[i], make_float2(s, s));
     f[2 * i] = q[i].x, f[2 * i + 1] = q[i].y;
-  }
-  if (scale >= kScaleTop8) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) asm("min.NaN.xorsign.abs.f32 %0, %0, 0f7F7FFFFF;" : "+f"(f[i]));
   }
 }
 
