@@ -126,8 +126,9 @@ __device__ __forceinline__ void activation_pair(float2 x, float2& f, float2& df)
     // x Phi(x) = max(x, 0) - |x| tail
     f = fma2(make_float2(-ax.x, -ax.y), tail, make_float2(fmaxf(x.x, 0.0f), fmaxf(x.y, 0.0f)));
     if constexpr (kDeriv) {
-      const float2 upper = fma2(tail, make_float2(-1.0f, -1.0f), one);
-      const float2 cdf = make_float2(x.x < 0.0f ? tail.x : upper.x, x.y < 0.0f ? tail.y : upper.y);
+      // tail below 0, 1 - tail above (and 1/2 where the step is neither 0 nor 1); on the FP32 pipe
+      const float2 step = make_float2(__saturatef(x.x * 1e38f), __saturatef(x.y * 1e38f));
+      const float2 cdf = fma2(tail, fma2(step, make_float2(-2.0f, -2.0f), one), step);
       df = fma2(mul2(x, g), make_float2(0.3989422804f, 0.3989422804f), cdf);
     }
   } else {
