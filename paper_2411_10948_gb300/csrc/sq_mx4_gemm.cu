@@ -817,6 +817,8 @@ static int launch_pair(Mx4Gemm& g, const Mx4Operand& a, const Mx4Operand& b, int
 }
 
 constexpr int kQuantRows = 32;   // rows that a product quantizes itself
+// whether a product takes the form of few rows: its column tiles are the grid's y
+static bool few_rows(int64_t M, int64_t N) { return M <= kQuantRows && (N + 127) / 128 <= 65535; }
 
 // rows: null where both operands are mx4
 template <typename T, int kN, bool kQuant>
@@ -841,10 +843,15 @@ static int launch_split(Mx4Gemm& g, const Mx4Operand& a, const Mx4Rows* rows, co
 
 template <typename T>
 static int run_mx4(Mx4Gemm& g, const Mx4Operand& a, const Mx4Operand& b, int64_t K, int dev, int sms, cudaStream_t s) {
+  // few rows in the form, and so with the order of sums, of rows that the product quantizes itself; as CTA
+  // pairs 32 rows through 4096 x 11008 took 16.4 us for 14.3 (a call alone), 4096 x 65536 43 for 37, 16 rows
+  // through 512 x 131072 18.4 for 20.4
+  if (few_rows(g.M, g.N)) {
+    if (g.M <= 16) return launch_split<T, 16, false>(g, a, nullptr, b, K, dev, sms, s);
+    return launch_split<T, 32, false>(g, a, nullptr, b, K, dev, sms, s);
+  }
   const int64_t tiles = ((g.M + 255) / 256) * ((g.N + 255) / 256);
   if (tiles >= sms / 4) return launch_pair<T>(g, a, b, K, dev, sms, s);
-  if (g.M <= 16) return launch_split<T, 16, false>(g, a, nullptr, b, K, dev, sms, s);
-  if (g.M <= 32) return launch_split<T, 32, false>(g, a, nullptr, b, K, dev, sms, s);
   // 128 rows where their blocks, each with a K range of a stage at least, fill the SMs, else 64.  No fewer
   // where there are several tiles: a scale operand starts at an even column of tensor memory
   // (32 rows each), so a tile of 16 or 32 rows can only be its scale tile's first.
@@ -935,7 +942,7 @@ extern "C" sq_status shiftquant_mx4_linear(const void* x, int dtype, int64_t M, 
   if (K == 0) return zero_output(y, M, N, ld_y, esize, s);
   if (x == nullptr || ld_x < K) return fail(SQ_EINVAL, "mx4_linear: NULL x or ld_x < K");
   if (reinterpret_cast<uintptr_t>(x) % esize) return fail(SQ_EALIGN, "mx4_linear: x is not aligned to its type");
-  if (M > kQuantRows || ((N + 255) / 256) >= (int64_t(1) << 15)) {
+  if (!few_rows(M, N)) {
     if (x_codes == nullptr || x_scales == nullptr)
       return fail(SQ_EINVAL, "mx4_linear: more than %d rows need x_codes and x_scales", kQuantRows);
     st = shiftquant_mx4_quantize(x, dtype, M, K, ld_x, SQ_ROUND_NEAREST_EVEN, 0, 0, x_codes, ld_x_codes, x_scales, nullptr, 0,
