@@ -677,8 +677,8 @@ sq_status shiftquant_mx4_linear(const void *x, int dtype, int64_t M, int64_t K, 
  * Arithmetic is FP32 (a row whose squares it does not hold, from 1.8e19 on, has reciprocal
  * deviation 0); each output is rounded once, to `dtype`.  Tensors may have any leading
  * dimension and their type's alignment; rows of 16-byte alignment are handled faster.  Forward
- * calls without codes (NULL, with scales and stats) keep nothing.  Outputs may not overlap inputs.
- * rows or cols == 0 is allowed; either above 2^30 returns SQ_EUNSUPPORTED.
+ * calls without codes (NULL, with scales and stats) keep nothing.  Outputs may not overlap inputs,
+ * but for norm8's sum and dx.  rows or cols == 0 is allowed; either above 2^30 returns SQ_EUNSUPPORTED.
  *
  * shiftquant_act8_forward: y [rows, cols] = f(h), h [rows, cols], f by sq_act; gated != 0: h has
  *   2 cols columns [a | u], y = f(a) u, and codes (scales) hold u's blocks behind a's, from
@@ -696,7 +696,8 @@ sq_status shiftquant_act8_backward(const void *dy, int dtype, int64_t rows, int6
                                    void *dh, int64_t ld_dh, void *stream);
 
 /* shiftquant_norm8_forward: normalization of the rows of s = x, or of s = x + residual rounded to
- *   `dtype` and written to sum (residual and sum NULL or both given):
+ *   `dtype` and written to sum (residual and sum NULL or both given; sum may be the residual itself,
+ *   at its address and leading dimension):
  *   beta given:  layer norm, y = (s - mean) / sqrt(var + eps) gamma + beta;
  *   beta NULL:   root-mean-square norm, y = s / sqrt(mean(s^2) + eps) gamma.
  *   s is kept as codes and scales; stats [rows][2] (fp32, 8-byte aligned) receive the mean (0 for
@@ -704,7 +705,7 @@ sq_status shiftquant_act8_backward(const void *dy, int dtype, int64_t rows, int6
  * shiftquant_norm8_backward: with xh = (s~ - mean) rstd and t = dy gamma,
  *   dx = rstd (t - mean(t) - xh mean(t xh)) (mean(t) in the layer norm alone), plus dsum [rows,
  *   cols] where given: the gradient that reaches s another way, as x's and the residual's are the
- *   same.  dgamma[cols] = sum over rows of dy xh; dbeta[cols] = sum of dy, NULL for the
+ *   same (dx may be dsum itself, at its address and leading dimension).  dgamma[cols] = sum over rows of dy xh; dbeta[cols] = sum of dy, NULL for the
  *   root-mean-square norm.  workspace: shiftquant_norm8_workspace_bytes(rows, cols) bytes for
  *   the current device, 16-byte aligned; sums are taken in a fixed order. */
 sq_status shiftquant_norm8_forward(const void *x, int dtype, int64_t rows, int64_t cols,

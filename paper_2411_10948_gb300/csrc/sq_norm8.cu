@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(512, kVec && kBlock && kChunks == 2 && sizeof(
   const int chunks = kChunks > 0 ? kChunks : static_cast<int>((a.C + 8 * G - 1) / (8 * G));
   const float inv_c = 1.0f / static_cast<float>(a.C);
   float v[kChunks > 0 ? kChunks : 1][8];
-  auto add = [&](RowIn<T, kVec>& in, float (&f)[8], int64_t c, bool store) {   // s = x + residual, rounded to the type
+  auto add = [&](RowIn<T, kVec>& in, float (&f)[8], int64_t c) {   // s = x + residual, rounded to the type
     float g[8];
     in.values(g, buf, lane);
 #pragma unroll
@@ -156,17 +156,19 @@ __global__ void __launch_bounds__(512, kVec && kBlock && kChunks == 2 && sizeof(
     Raw8<T> w;
     round8(w, f);
     values8<T>(w, f);
-    if (!store) return;
     if (kVec && c + 8 <= a.C) store8(sum + c, w);
     else row_store<T, kVec>(sum, f, c, a.C, true, buf, lane);
   };
-  auto fetch = [&](int k, float (&f)[8], bool first) {   // s of a chunk
+  // s of a chunk; after the first sweep the sum is read back (each thread its own elements), as it may have
+  // taken the residual's place
+  auto fetch = [&](int k, float (&f)[8], bool first) {
     RowIn<T, kVec> in, rr;
     const int64_t c = norm_col(k, t, G);
-    in.load(x, c, a.C, true, lane);
-    if (res != nullptr) rr.load(res, c, a.C, true, lane);
+    const bool adds = res != nullptr && first;
+    in.load(res != nullptr && !first ? sum : x, c, a.C, true, lane);
+    if (adds) rr.load(res, c, a.C, true, lane);
     in.values(f, buf, lane);
-    if (res != nullptr) add(rr, f, c, first);
+    if (adds) add(rr, f, c);
   };
   float2 acc = make_float2(0.0f, 0.0f);
   if constexpr (kChunks > 0) {
@@ -180,7 +182,7 @@ __global__ void __launch_bounds__(512, kVec && kBlock && kChunks == 2 && sizeof(
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
       in[k].values(v[k], buf, lane);
-      if (res != nullptr) add(rr[k], v[k], norm_col(k, t, G), true);
+      if (res != nullptr) add(rr[k], v[k], norm_col(k, t, G));
     }
   }
   auto chunk = [&](int k, float (&f)[8], bool first) {

@@ -160,7 +160,8 @@ ACTIVATIONS = {"gelu": N.SQ_ACT_GELU, "gelu_tanh": N.SQ_ACT_GELU_TANH, "silu": N
 class Act8:
     """y = f(h) of h [M, F], or gated y = f(a) u of h = [a | u] [M, 2 F]; h is kept in 8 bits
     for the backward pass (33 bytes per 32 elements).  The object owns y and dh, whose addresses
-    its calls pass; with train=False it keeps nothing.  Both calls take up to M rows."""
+    its calls pass, and which may not be the same call's input; with train=False it keeps nothing.
+    Both calls take up to M rows."""
 
     def __init__(self, M: int, F: int, dtype: torch.dtype, act: str, gated: bool, device, train: bool = True):
         if act not in ACTIVATIONS:
@@ -202,7 +203,8 @@ class Act8:
 class Norm8:
     """Layer norm ("layer") or root-mean-square norm ("rms") of the rows of x [M, C], or of
     x + residual, whose input is kept in 8 bits for the backward pass.  The object owns the
-    outputs, whose addresses its calls pass; both calls take up to M rows."""
+    outputs, whose addresses its calls pass; both calls take up to M rows.  A call's inputs may not
+    be its own outputs, but for the residual stream in place: residual = sum, and dsum = dx."""
 
     def __init__(self, M: int, C: int, dtype: torch.dtype, norm: str, device, residual: bool = False,
                  eps: float = 1e-5, train: bool = True):
