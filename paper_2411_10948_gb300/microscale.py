@@ -88,6 +88,7 @@ class Mx4Linear:
 
     def __init__(self, M: int, K: int, Nout: int, dtype: torch.dtype, device, train: bool = True):
         self.M, self.K, self.N, self.train = M, K, Nout, train
+        self._rows = None              # of the last forward call whose codes are kept
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.x = Mx4Tensor.alloc(M, K, device, True, train, self.status)
         self.w = Mx4Tensor.alloc(K, Nout, device, train, True, self.status)
@@ -128,6 +129,7 @@ class Mx4Linear:
                 status = lib.shiftquant_mx4_gemm(*self._forward, m, self.N, k, self._y[0], self._dtype, self._y[1],
                                                  self._status, s)
         N._check(status)
+        self._rows = m if self.train else None
         return self.y if m == self.M else self.y[:m]
 
     def backward(self, dy: torch.Tensor, seed: int, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
@@ -135,6 +137,7 @@ class Mx4Linear:
         m, n = dy.shape
         if (m, n) != (self.M, self.N):
             raise ValueError(f"dy of [{self.M}, {self.N}] expected, not {(m, n)}")
+        _require_kept(m, self._rows)
         lib, s = self._lib, N._stream(stream)
         status = lib.shiftquant_mx4_quantize(dy.data_ptr(), N._dtype(dy), m, n, N._ld(dy), N.SQ_ROUND_STOCHASTIC,
                                              seed & (2**64 - 1), 0, *self._quantize_g, s)
@@ -144,6 +147,14 @@ class Mx4Linear:
             status = lib.shiftquant_mx4_gemm(*self._dw, s)
         N._check(status)
         return self.dx, self.dw
+
+
+def _require_kept(rows: int, kept: int | None) -> None:
+    """A backward pass takes the rows of the last forward pass, whose codes are what is kept."""
+    if rows != kept:
+        raise ValueError(f"a gradient of {rows} rows, where " +
+                         ("no forward pass has kept its input" if kept is None
+                          else f"the last forward pass kept {kept}"))
 
 
 def _kept(rows: int, cols: int, parts: int, device) -> tuple[torch.Tensor, torch.Tensor]:
@@ -170,6 +181,7 @@ class Act8:
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.y = torch.zeros((M, F), dtype=dtype, device=device)
         self.codes = self.scales = self.dh = None
+        self.train, self._rows = train, None
         if train:
             self.codes, self.scales = _kept(M, F, self.parts, device)
             self.dh = torch.zeros((M, self.parts * F), dtype=dtype, device=device)
@@ -190,11 +202,13 @@ class Act8:
         m = self._check(h, self.parts * self.F)
         N._check(self._lib.shiftquant_act8_forward(h.data_ptr(), self._dtype, m, self.F, N._ld(h), *self._forward,
                                                    N._stream(stream)))
+        self._rows = m if self.train else None
         return self.y if m == self.M else self.y[:m]
 
     def backward(self, dy: torch.Tensor, stream=None) -> torch.Tensor:
-        """dh from dy and the input the last forward kept."""
+        """dh from dy and the input the last forward kept (as many rows)."""
         m = self._check(dy, self.F)
+        _require_kept(m, self._rows)
         N._check(self._lib.shiftquant_act8_backward(dy.data_ptr(), self._dtype, m, self.F, N._ld(dy), *self._backward,
                                                     N._stream(stream)))
         return self.dh if m == self.M else self.dh[:m]
@@ -215,6 +229,7 @@ class Norm8:
         self.y = torch.zeros((M, C), dtype=dtype, device=device)
         self.sum = torch.zeros((M, C), dtype=dtype, device=device) if residual else None
         self.codes = self.scales = self.stats = None
+        self.train, self._rows = train, None
         if train:
             self.codes, self.scales = _kept(M, C, 1, device)
             self.stats = torch.zeros((M, 2), dtype=torch.float32, device=device)
@@ -257,14 +272,16 @@ class Norm8:
         N._check(self._lib.shiftquant_norm8_forward(
             x.data_ptr(), self._dtype, m, self.C, N._ld(x), *res, *self._sum, self._param(gamma),
             0 if beta is None else self._param(beta), *self._forward, N._stream(stream)))
+        self._rows = m if self.train else None
         if m == self.M:
             return self.y, self.sum
         return self.y[:m], None if self.sum is None else self.sum[:m]
 
     def backward(self, dy: torch.Tensor, gamma: torch.Tensor, dsum: torch.Tensor | None = None, stream=None):
         """dx (with dsum, the gradient that reaches the sum another way, added), dgamma and dbeta
-        (None for the root-mean-square norm)."""
+        (None for the root-mean-square norm), of as many rows as the last forward kept."""
         m = self._check(dy, dsum)
+        _require_kept(m, self._rows)
         ds = (0, 0) if dsum is None else (dsum.data_ptr(), N._ld(dsum))
         N._check(self._lib.shiftquant_norm8_backward(
             dy.data_ptr(), self._dtype, m, self.C, N._ld(dy), *self._backward, self._param(gamma), *ds, *self._grads,
