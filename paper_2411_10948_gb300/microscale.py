@@ -18,6 +18,12 @@ def _blocks(rows: int, cols: int, device) -> tuple[torch.Tensor, torch.Tensor]:
     return codes, scales
 
 
+def _require_device(t: torch.Tensor, own: torch.Tensor) -> None:
+    """Kernels take addresses: a tensor of another device than the object's has none of its own."""
+    if t.device != own.device:
+        raise ValueError(f"a tensor on {own.device} expected, not on {t.device}")
+
+
 @dataclass
 class Mx4Tensor:
     """A [R, C] tensor in mx4: codes and scales along its rows, and of its transpose."""
@@ -59,6 +65,7 @@ class Mx4Tensor:
         """Both orientations this tensor holds from x, in one pass."""
         if x.shape != self.shape:
             raise ValueError(f"a tensor of {self.shape}, not {tuple(x.shape)}")
+        _require_device(x, self.status)
         N._check(N.load().shiftquant_mx4_quantize(
             x.data_ptr(), N._dtype(x), *self.shape, N._ld(x),
             N.SQ_ROUND_STOCHASTIC if stochastic else N.SQ_ROUND_NEAREST_EVEN, seed & (2**64 - 1), row0, *self._own,
@@ -69,6 +76,7 @@ class Mx4Tensor:
         """The values the codes along the rows stand for, into out [R, C]."""
         if tuple(out.shape) != self.shape:
             raise ValueError(f"an output of {self.shape}, not {tuple(out.shape)}")
+        _require_device(out, self.status)
         N.shiftquant_mx4_dequantize(self.codes, self.scales, out, stream)
         return out
 
@@ -76,6 +84,7 @@ class Mx4Tensor:
         """The same of the transpose, into out [C, R]."""
         if tuple(out.shape) != self.shape[::-1]:
             raise ValueError(f"an output of {self.shape[::-1]}, not {tuple(out.shape)}")
+        _require_device(out, self.status)
         N.shiftquant_mx4_dequantize(self.codes_t, self.scales_t, out, stream)
         return out
 
@@ -119,6 +128,7 @@ class Mx4Linear:
         m, k = x.shape
         if k != self.K or (m != self.M if self.train else m > self.M):
             raise ValueError(f"x of [{self.M}, {self.K}] expected, not {(m, k)}")
+        _require_device(x, self.y)
         lib, s, dtype = self._lib, N._stream(stream), N._dtype(x)
         if not self.train and dtype == self._dtype:
             status = lib.shiftquant_mx4_linear(x.data_ptr(), dtype, m, k, N._ld(x), *self._serve, s)
@@ -137,6 +147,7 @@ class Mx4Linear:
         m, n = dy.shape
         if (m, n) != (self.M, self.N):
             raise ValueError(f"dy of [{self.M}, {self.N}] expected, not {(m, n)}")
+        _require_device(dy, self.y)
         _require_kept(m, self._rows)
         lib, s = self._lib, N._stream(stream)
         status = lib.shiftquant_mx4_quantize(dy.data_ptr(), N._dtype(dy), m, n, N._ld(dy), N.SQ_ROUND_STOCHASTIC,
@@ -196,6 +207,7 @@ class Act8:
             raise ValueError(f"a tensor of [{self.M}, {cols}] expected, not {(m, c)}")
         if t.dtype != self.y.dtype:
             raise TypeError(f"a tensor of {self.y.dtype} expected, not {t.dtype}")
+        _require_device(t, self.y)
         return m
 
     def forward(self, h: torch.Tensor, stream=None) -> torch.Tensor:
@@ -253,13 +265,17 @@ class Norm8:
             raise ValueError(f"a tensor of [{self.M}, {self.C}] expected, not {(m, c)}")
         if x.dtype != self.y.dtype:
             raise TypeError(f"a tensor of {self.y.dtype} expected, not {x.dtype}")
-        if other is not None and (other.shape != x.shape or other.dtype != x.dtype):
-            raise ValueError(f"tensors of one shape and type expected, not {(m, c)} and {tuple(other.shape)}")
+        _require_device(x, self.y)
+        if other is not None:
+            if other.shape != x.shape or other.dtype != x.dtype:
+                raise ValueError(f"tensors of one shape and type expected, not {(m, c)} and {tuple(other.shape)}")
+            _require_device(other, self.y)
         return m
 
     def _param(self, p: torch.Tensor) -> int:
         if p.shape != (self.C,) or p.dtype != torch.float32 or not p.is_contiguous():
             raise ValueError(f"gamma and beta are fp32 vectors of {self.C}")
+        _require_device(p, self.y)
         return p.data_ptr()
 
     def forward(self, x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor | None = None,
