@@ -92,8 +92,8 @@ class Mx4Tensor:
 class Mx4Linear:
     """Y = X W with X [M, K] and W [K, N] in mx4: nearest-even forward operands, stochastic
     gradients.  The layer owns its outputs y, dx (of `dtype`) and dw (fp32), whose addresses its
-    calls pass; with train=False it holds the forward weight alone and takes up to M tokens at
-    a time."""
+    calls pass; with train=False it holds the forward weight alone.  Calls take up to M rows, and
+    the codes of x and dy are laid out for the last call's."""
 
     def __init__(self, M: int, K: int, Nout: int, dtype: torch.dtype, device, train: bool = True):
         self.M, self.K, self.N, self.train = M, K, Nout, train
@@ -117,16 +117,17 @@ class Mx4Linear:
         if train:
             g = self.g
             self._quantize_g = g.arguments()
-            self._dx = (*g.operand(), *w.operand(), M, K, Nout, self.dx.data_ptr(), self._dtype, K, self._status)
-            self._dw = (*x.operand_t(), *g.operand_t(), K, Nout, M, self.dw.data_ptr(), N.SQ_F32, Nout, self._status)
+            # ... and what follows the number of rows
+            self._dx = (*g.operand(), *w.operand()), (K, Nout, self.dx.data_ptr(), self._dtype, K, self._status)
+            self._dw = (*x.operand_t(), *g.operand_t(), K, Nout), (self.dw.data_ptr(), N.SQ_F32, Nout, self._status)
 
     def set_weight(self, w: torch.Tensor, stream=None) -> None:
         self.w.quantize(w, stream=stream)
 
     def forward(self, x: torch.Tensor, stream=None) -> torch.Tensor:
-        """y [tokens, N]; x's codes stay for the backward pass."""
+        """y [rows of x, N]; x's codes stay for the backward pass."""
         m, k = x.shape
-        if k != self.K or (m != self.M if self.train else m > self.M):
+        if k != self.K or m > self.M:
             raise ValueError(f"x of [{self.M}, {self.K}] expected, not {(m, k)}")
         _require_device(x, self.y)
         lib, s, dtype = self._lib, N._stream(stream), N._dtype(x)
@@ -143,9 +144,9 @@ class Mx4Linear:
         return self.y if m == self.M else self.y[:m]
 
     def backward(self, dy: torch.Tensor, seed: int, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
-        """dx and dw from dy [M, N] and the codes the last forward left."""
+        """dx and dw from dy and the codes the last forward left (of as many rows)."""
         m, n = dy.shape
-        if (m, n) != (self.M, self.N):
+        if n != self.N or m > self.M:
             raise ValueError(f"dy of [{self.M}, {self.N}] expected, not {(m, n)}")
         _require_device(dy, self.y)
         _require_kept(m, self._rows)
@@ -153,11 +154,13 @@ class Mx4Linear:
         status = lib.shiftquant_mx4_quantize(dy.data_ptr(), N._dtype(dy), m, n, N._ld(dy), N.SQ_ROUND_STOCHASTIC,
                                              seed & (2**64 - 1), 0, *self._quantize_g, s)
         if status == N.SQ_OK:
-            status = lib.shiftquant_mx4_gemm(*self._dx, s)
+            operands, rest = self._dx
+            status = lib.shiftquant_mx4_gemm(*operands, m, *rest, s)
         if status == N.SQ_OK:
-            status = lib.shiftquant_mx4_gemm(*self._dw, s)
+            operands, rest = self._dw
+            status = lib.shiftquant_mx4_gemm(*operands, m, *rest, s)
         N._check(status)
-        return self.dx, self.dw
+        return self.dx if m == self.M else self.dx[:m], self.dw
 
 
 def _require_kept(rows: int, kept: int | None) -> None:
