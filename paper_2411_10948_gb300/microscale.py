@@ -24,6 +24,16 @@ def _require_device(t: torch.Tensor, own: torch.Tensor) -> None:
         raise ValueError(f"a tensor on {own.device} expected, not on {t.device}")
 
 
+def _require_alike(new, share, what: tuple[str, ...]) -> None:
+    """An object shares buffers with one that was made alike."""
+    for name in what:
+        if getattr(new, name) != getattr(share, name):
+            raise ValueError(f"buffers are shared with an object of the same {name}: "
+                             f"{getattr(share, name)}, not {getattr(new, name)}")
+    if new.status.device != share.status.device:
+        raise ValueError(f"buffers are shared on one device: {share.status.device}, not {new.status.device}")
+
+
 @dataclass
 class Mx4Tensor:
     """A [R, C] tensor in mx4: codes and scales along its rows, and of its transpose."""
@@ -93,19 +103,35 @@ class Mx4Linear:
     """Y = X W with X [M, K] and W [K, N] in mx4: nearest-even forward operands, stochastic
     gradients.  The layer owns its outputs y, dx (of `dtype`) and dw (fp32), whose addresses its
     calls pass; with train=False it holds the forward weight alone.  Calls take up to M rows, and
-    the codes of x and dy are laid out for the last call's."""
+    the codes of x and dy are laid out for the last call's.
 
-    def __init__(self, M: int, K: int, Nout: int, dtype: torch.dtype, device, train: bool = True):
-        self.M, self.K, self.N, self.train = M, K, Nout, train
+    share: a layer made alike, whose buffers of what does not outlast a call's use this one takes
+    too (y, dx, the codes of dy and those of x for the forward product); its own are the weight, what
+    the backward pass needs of x, and dw.  An output of either then stays until the next call of
+    the same kind of any of them, and their calls are in order on one stream."""
+
+    def __init__(self, M: int, K: int, Nout: int, dtype: torch.dtype, device, train: bool = True,
+                 share: "Mx4Linear | None" = None):
+        self.M, self.K, self.N, self.dtype, self.train = M, K, Nout, dtype, train
         self._rows = None              # of the last forward call whose codes are kept
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
-        self.x = Mx4Tensor.alloc(M, K, device, True, train, self.status)
         self.w = Mx4Tensor.alloc(K, Nout, device, train, True, self.status)
-        self.y = torch.zeros((M, Nout), dtype=dtype, device=device)
         self.dx = self.dw = None
+        if share is None:
+            self.x = Mx4Tensor.alloc(M, K, device, True, train, self.status)
+            self.y = torch.zeros((M, Nout), dtype=dtype, device=device)
+        else:
+            _require_alike(self, share, ("M", "K", "N", "dtype", "train"))
+            codes_t, scales_t = _blocks(K, M, device) if train else (None, None)
+            self.x = Mx4Tensor((M, K), share.x.codes, share.x.scales, codes_t, scales_t, self.status)
+            self.y = share.y
         if train:
-            self.g = Mx4Tensor.alloc(M, Nout, device, True, True, self.status)
-            self.dx = torch.zeros((M, K), dtype=dtype, device=device)
+            if share is None:
+                self.g = Mx4Tensor.alloc(M, Nout, device, True, True, self.status)
+                self.dx = torch.zeros((M, K), dtype=dtype, device=device)
+            else:
+                g, self.dx = share.g, share.dx
+                self.g = Mx4Tensor((M, Nout), g.codes, g.scales, g.codes_t, g.scales_t, self.status)
             self.dw = torch.zeros((K, Nout), dtype=torch.float32, device=device)
         self._lib, self._dtype, self._status = N.load(), N._dtype(self.y), self.status.data_ptr()
         x, w = self.x, self.w
@@ -186,19 +212,26 @@ class Act8:
     """y = f(h) of h [M, F], or gated y = f(a) u of h = [a | u] [M, 2 F]; h is kept in 8 bits
     for the backward pass (33 bytes per 32 elements).  The object owns y and dh, whose addresses
     its calls pass, and which may not be the same call's input; with train=False it keeps nothing.
-    Both calls take up to M rows."""
+    Both calls take up to M rows.  share: an object made alike, whose y and dh this one takes too:
+    they stay until the next call of either, and calls are in order on one stream."""
 
-    def __init__(self, M: int, F: int, dtype: torch.dtype, act: str, gated: bool, device, train: bool = True):
+    def __init__(self, M: int, F: int, dtype: torch.dtype, act: str, gated: bool, device, train: bool = True,
+                 share: "Act8 | None" = None):
         if act not in ACTIVATIONS:
             raise ValueError(f"an activation of {sorted(ACTIVATIONS)}, not {act!r}")
-        self.M, self.F, self.parts, self.act = M, F, 2 if gated else 1, ACTIVATIONS[act]
+        self.M, self.F, self.dtype, self.parts, self.act = M, F, dtype, 2 if gated else 1, ACTIVATIONS[act]
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
-        self.y = torch.zeros((M, F), dtype=dtype, device=device)
         self.codes = self.scales = self.dh = None
         self.train, self._rows = train, None
+        if share is None:
+            self.y = torch.zeros((M, F), dtype=dtype, device=device)
+            if train:
+                self.dh = torch.zeros((M, self.parts * F), dtype=dtype, device=device)
+        else:
+            _require_alike(self, share, ("M", "F", "dtype", "parts", "train"))
+            self.y, self.dh = share.y, share.dh
         if train:
             self.codes, self.scales = _kept(M, F, self.parts, device)
-            self.dh = torch.zeros((M, self.parts * F), dtype=dtype, device=device)
         self._lib, self._dtype = N.load(), N._dtype(self.y)
         kept = (*N._fixed(self.codes), *N._fixed(self.scales))
         self._forward = (self.act, self.parts - 1, *N._fixed(self.y), *kept, self.status.data_ptr())
@@ -233,26 +266,35 @@ class Norm8:
     """Layer norm ("layer") or root-mean-square norm ("rms") of the rows of x [M, C], or of
     x + residual, whose input is kept in 8 bits for the backward pass.  The object owns the
     outputs, whose addresses its calls pass; both calls take up to M rows.  A call's inputs may not
-    be its own outputs, but for the residual stream in place: residual = sum, and dsum = dx."""
+    be its own outputs, but for the residual stream in place: residual = sum, and dsum = dx.
+    share: an object made alike, whose y, sum, dx and workspace this one takes too: they stay until
+    the next call of either, and calls are in order on one stream."""
 
     def __init__(self, M: int, C: int, dtype: torch.dtype, norm: str, device, residual: bool = False,
-                 eps: float = 1e-5, train: bool = True):
+                 eps: float = 1e-5, train: bool = True, share: "Norm8 | None" = None):
         if norm not in ("layer", "rms"):
             raise ValueError(f"a norm of 'layer' and 'rms', not {norm!r}")
-        self.M, self.C, self.layer, self.eps = M, C, norm == "layer", eps
-        self.status = torch.zeros(1, dtype=torch.int32, device=device)
-        self.y = torch.zeros((M, C), dtype=dtype, device=device)
-        self.sum = torch.zeros((M, C), dtype=dtype, device=device) if residual else None
-        self.codes = self.scales = self.stats = None
+        self.M, self.C, self.dtype, self.layer, self.residual, self.eps = M, C, dtype, norm == "layer", residual, eps
         self.train, self._rows = train, None
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        if share is None:
+            self.y = torch.zeros((M, C), dtype=dtype, device=device)
+            self.sum = torch.zeros((M, C), dtype=dtype, device=device) if residual else None
+        else:
+            _require_alike(self, share, ("M", "C", "dtype", "residual", "train"))
+            self.y, self.sum = share.y, share.sum
+        self.codes = self.scales = self.stats = None
         if train:
             self.codes, self.scales = _kept(M, C, 1, device)
             self.stats = torch.zeros((M, 2), dtype=torch.float32, device=device)
-            self.dx = torch.zeros((M, C), dtype=dtype, device=device)
             self.dgamma = torch.zeros(C, dtype=torch.float32, device=device)
             self.dbeta = torch.zeros(C, dtype=torch.float32, device=device) if self.layer else None
-            self.workspace = torch.zeros(max(N.shiftquant_norm8_workspace_bytes(M, C), 16), dtype=torch.uint8,
-                                         device=device)
+            if share is None:
+                self.dx = torch.zeros((M, C), dtype=dtype, device=device)
+                self.workspace = torch.zeros(max(N.shiftquant_norm8_workspace_bytes(M, C), 16), dtype=torch.uint8,
+                                             device=device)
+            else:
+                self.dx, self.workspace = share.dx, share.workspace
         self._lib, self._dtype = N.load(), N._dtype(self.y)
         kept = (*N._fixed(self.codes), *N._fixed(self.scales))
         self._sum = N._fixed(self.sum)
@@ -315,14 +357,22 @@ class Mx4MlpBlock:
 
     forward(delta, x): x_new = x + delta (the residual stream), out = W2 f(W1 norm(x_new)), which the
     next block adds.  backward(dout, dx_new) returns d(delta) = d(x) and leaves the weights'
-    gradients in dw1, dw2 and dgamma."""
+    gradients in dw1, dw2 and dgamma.
 
-    def __init__(self, M: int, C: int, F: int, dtype: torch.dtype, device, act: str = "silu", gated: bool = True):
+    share: a block made alike, whose buffers of what only one block at a time needs this one takes
+    too.  A chain of blocks that share with its first holds one set of them; x_new and the gradient
+    of the stream then pass along the chain in place, and a block's own are its weights, their
+    gradients, and the 8-bit and 4-bit codes that its backward pass needs.  Outputs stay until
+    the next block's call, and calls are in order on one stream."""
+
+    def __init__(self, M: int, C: int, F: int, dtype: torch.dtype, device, act: str = "silu", gated: bool = True,
+                 share: "Mx4MlpBlock | None" = None):
         parts = 2 if gated else 1
-        self.norm = Norm8(M, C, dtype, "rms", device, residual=True)
-        self.up = Mx4Linear(M, C, parts * F, dtype, device)
-        self.act = Act8(M, F, dtype, act, gated, device)
-        self.down = Mx4Linear(M, F, C, dtype, device)
+        norm, up, mid, down = (None,) * 4 if share is None else (share.norm, share.up, share.act, share.down)
+        self.norm = Norm8(M, C, dtype, "rms", device, residual=True, share=norm)
+        self.up = Mx4Linear(M, C, parts * F, dtype, device, share=up)
+        self.act = Act8(M, F, dtype, act, gated, device, share=mid)
+        self.down = Mx4Linear(M, F, C, dtype, device, share=down)
 
     def set_weights(self, gamma: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, stream=None) -> None:
         """gamma [C] (fp32, read at each call), w1 [C, F or 2 F], w2 [F, C]."""
