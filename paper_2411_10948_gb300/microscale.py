@@ -356,8 +356,9 @@ class Mx4MlpBlock:
     previous block's output folded into the norm.
 
     forward(delta, x): x_new = x + delta (the residual stream), out = W2 f(W1 norm(x_new)), which the
-    next block adds.  backward(dout, dx_new) returns d(delta) = d(x) and leaves the weights'
-    gradients in dw1, dw2 and dgamma.
+    next block adds.  backward(dout, dx_new, seed) returns d(delta) = d(x) and leaves the weights'
+    gradients in dw1, dw2 and dgamma.  It takes the draws of seed for dout and of seed + 1 for the
+    gradient between the products: calls whose draws are not to meet have seeds two apart or more.
 
     share: a block made alike, whose buffers of what only one block at a time needs this one takes
     too.  A chain of blocks that share with its first holds one set of them; x_new and the gradient
