@@ -649,7 +649,8 @@ sq_status shiftquant_mx4_dequantize(const uint8_t *codes, int64_t ld_codes,
  *   forward          a = codes of X,     b = codes_t of W
  *   loss propagation a = codes of dY,    b = codes of W
  *   weight gradient  a = codes_t of X,   b = codes_t of dY
- * One launch, no workspace; results do not depend on the device's load.  K = 0 gives zeros. */
+ * One launch, no workspace; results do not depend on the device's load, but the order of the FP32
+ * sums, and so their rounding, follows from the sizes and the device's SMs.  K = 0 gives zeros. */
 sq_status shiftquant_mx4_gemm(const uint8_t *a_codes, int64_t lda, const uint8_t *a_scales,
                               const uint8_t *b_codes, int64_t ldb, const uint8_t *b_scales,
                               int64_t M, int64_t N, int64_t K, void *d, int dtype, int64_t ldd,
