@@ -131,7 +131,7 @@ __device__ __forceinline__ float2 row_sum(float2 v, RowRed<kTwo>& all, int& half
 // rounded sum is stored as it is read back: element by element these took 92, 148 and 25 us.  (One wave of blocks that walk the rows, the next row on its way: 64 registers spill, more
 // leave too few warps; 16384 x 4096 bf16 99 us.)
 template <typename T, int kChunks, bool kVec, bool kBlock, bool kLayer>
-__global__ void __launch_bounds__(512, kVec && kBlock && kChunks == 2 && sizeof(T) == 2 ? (kLayer ? 2 : 3) : 1) norm8_forward_kernel(const Norm8Args a) {
+__global__ void __launch_bounds__(512, kVec && kBlock && kChunks == 2 && sizeof(T) == 2 && !kLayer ? 3 : 1) norm8_forward_kernel(const Norm8Args a) {
   __shared__ RowRed<false> red;
   __shared__ __align__(16) T exchange[kVec ? 1 : 16][kVec ? 8 : 256];
   int half = 0;
