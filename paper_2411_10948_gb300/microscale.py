@@ -18,10 +18,9 @@ def _blocks(rows: int, cols: int, device) -> tuple[torch.Tensor, torch.Tensor]:
     return codes, scales
 
 
-def _require_device(t: torch.Tensor, own: torch.Tensor) -> None:
-    """Kernels take addresses: a tensor of another device than the object's has none of its own."""
-    if t.device != own.device:
-        raise ValueError(f"a tensor on {own.device} expected, not on {t.device}")
+def _elsewhere(t: torch.Tensor, device: torch.device) -> ValueError:
+    """Kernels take addresses: a tensor of another device than the object's (`_on`) has none of its own."""
+    return ValueError(f"a tensor on {device} expected, not on {t.device}")
 
 
 def _require_alike(new, share, what: tuple[str, ...]) -> None:
@@ -46,6 +45,7 @@ class Mx4Tensor:
 
     def __post_init__(self):
         self._own = self.arguments()   # the tensor's buffers stay
+        self._on = self.status.device
 
     @staticmethod
     def alloc(R: int, C: int, device, rows: bool = True, cols: bool = True,
@@ -75,7 +75,8 @@ class Mx4Tensor:
         """Both orientations this tensor holds from x, in one pass."""
         if x.shape != self.shape:
             raise ValueError(f"a tensor of {self.shape}, not {tuple(x.shape)}")
-        _require_device(x, self.status)
+        if x.device != self._on:
+            raise _elsewhere(x, self._on)
         N._check(N.load().shiftquant_mx4_quantize(
             x.data_ptr(), N._dtype(x), *self.shape, N._ld(x),
             N.SQ_ROUND_STOCHASTIC if stochastic else N.SQ_ROUND_NEAREST_EVEN, seed & (2**64 - 1), row0, *self._own,
@@ -86,7 +87,8 @@ class Mx4Tensor:
         """The values the codes along the rows stand for, into out [R, C]."""
         if tuple(out.shape) != self.shape:
             raise ValueError(f"an output of {self.shape}, not {tuple(out.shape)}")
-        _require_device(out, self.status)
+        if out.device != self._on:
+            raise _elsewhere(out, self._on)
         N.shiftquant_mx4_dequantize(self.codes, self.scales, out, stream)
         return out
 
@@ -94,7 +96,8 @@ class Mx4Tensor:
         """The same of the transpose, into out [C, R]."""
         if tuple(out.shape) != self.shape[::-1]:
             raise ValueError(f"an output of {self.shape[::-1]}, not {tuple(out.shape)}")
-        _require_device(out, self.status)
+        if out.device != self._on:
+            raise _elsewhere(out, self._on)
         N.shiftquant_mx4_dequantize(self.codes_t, self.scales_t, out, stream)
         return out
 
@@ -134,6 +137,7 @@ class Mx4Linear:
                 self.g = Mx4Tensor((M, Nout), g.codes, g.scales, g.codes_t, g.scales_t, self.status)
             self.dw = torch.zeros((K, Nout), dtype=torch.float32, device=device)
         self._lib, self._dtype, self._status = N.load(), N._dtype(self.y), self.status.data_ptr()
+        self._on = self.status.device
         x, w = self.x, self.w
         self._quantize_x = x.arguments()
         self._y = N._fixed(self.y)
@@ -155,7 +159,8 @@ class Mx4Linear:
         m, k = x.shape
         if k != self.K or m > self.M:
             raise ValueError(f"x of [{self.M}, {self.K}] expected, not {(m, k)}")
-        _require_device(x, self.y)
+        if x.device != self._on:
+            raise _elsewhere(x, self._on)
         lib, s, dtype = self._lib, N._stream(stream), N._dtype(x)
         if not self.train and dtype == self._dtype:
             status = lib.shiftquant_mx4_linear(x.data_ptr(), dtype, m, k, N._ld(x), *self._serve, s)
@@ -174,8 +179,10 @@ class Mx4Linear:
         m, n = dy.shape
         if n != self.N or m > self.M:
             raise ValueError(f"dy of [{self.M}, {self.N}] expected, not {(m, n)}")
-        _require_device(dy, self.y)
-        _require_kept(m, self._rows)
+        if dy.device != self._on:
+            raise _elsewhere(dy, self._on)
+        if m != self._rows:
+            raise _not_kept(m, self._rows)
         lib, s = self._lib, N._stream(stream)
         status = lib.shiftquant_mx4_quantize(dy.data_ptr(), N._dtype(dy), m, n, N._ld(dy), N.SQ_ROUND_STOCHASTIC,
                                              seed & (2**64 - 1), 0, *self._quantize_g, s)
@@ -189,12 +196,11 @@ class Mx4Linear:
         return self.dx if m == self.M else self.dx[:m], self.dw
 
 
-def _require_kept(rows: int, kept: int | None) -> None:
+def _not_kept(rows: int, kept: int | None) -> ValueError:
     """A backward pass takes the rows of the last forward pass, whose codes are what is kept."""
-    if rows != kept:
-        raise ValueError(f"a gradient of {rows} rows, where " +
-                         ("no forward pass has kept its input" if kept is None
-                          else f"the last forward pass kept {kept}"))
+    return ValueError(f"a gradient of {rows} rows, where " +
+                      ("no forward pass has kept its input" if kept is None
+                       else f"the last forward pass kept {kept}"))
 
 
 def _kept(rows: int, cols: int, parts: int, device) -> tuple[torch.Tensor, torch.Tensor]:
@@ -232,7 +238,7 @@ class Act8:
             self.y, self.dh = share.y, share.dh
         if train:
             self.codes, self.scales = _kept(M, F, self.parts, device)
-        self._lib, self._dtype = N.load(), N._dtype(self.y)
+        self._lib, self._dtype, self._on = N.load(), N._dtype(self.y), self.status.device
         kept = (*N._fixed(self.codes), *N._fixed(self.scales))
         self._forward = (self.act, self.parts - 1, *N._fixed(self.y), *kept, self.status.data_ptr())
         self._backward = (*kept, self.act, self.parts - 1, *N._fixed(self.dh))
@@ -241,9 +247,10 @@ class Act8:
         m, c = t.shape
         if m > self.M or c != cols:
             raise ValueError(f"a tensor of [{self.M}, {cols}] expected, not {(m, c)}")
-        if t.dtype != self.y.dtype:
-            raise TypeError(f"a tensor of {self.y.dtype} expected, not {t.dtype}")
-        _require_device(t, self.y)
+        if t.dtype != self.dtype:
+            raise TypeError(f"a tensor of {self.dtype} expected, not {t.dtype}")
+        if t.device != self._on:
+            raise _elsewhere(t, self._on)
         return m
 
     def forward(self, h: torch.Tensor, stream=None) -> torch.Tensor:
@@ -256,7 +263,8 @@ class Act8:
     def backward(self, dy: torch.Tensor, stream=None) -> torch.Tensor:
         """dh from dy and the input the last forward kept (as many rows)."""
         m = self._check(dy, self.F)
-        _require_kept(m, self._rows)
+        if m != self._rows:
+            raise _not_kept(m, self._rows)
         N._check(self._lib.shiftquant_act8_backward(dy.data_ptr(), self._dtype, m, self.F, N._ld(dy), *self._backward,
                                                     N._stream(stream)))
         return self.dh if m == self.M else self.dh[:m]
@@ -295,7 +303,7 @@ class Norm8:
                                              device=device)
             else:
                 self.dx, self.workspace = share.dx, share.workspace
-        self._lib, self._dtype = N.load(), N._dtype(self.y)
+        self._lib, self._dtype, self._on = N.load(), N._dtype(self.y), self.status.device
         kept = (*N._fixed(self.codes), *N._fixed(self.scales))
         self._sum = N._fixed(self.sum)
         self._forward = (eps, *N._fixed(self.y), *kept, N._fixed(self.stats)[0], self.status.data_ptr())
@@ -308,19 +316,22 @@ class Norm8:
         m, c = x.shape
         if m > self.M or c != self.C:
             raise ValueError(f"a tensor of [{self.M}, {self.C}] expected, not {(m, c)}")
-        if x.dtype != self.y.dtype:
-            raise TypeError(f"a tensor of {self.y.dtype} expected, not {x.dtype}")
-        _require_device(x, self.y)
+        if x.dtype != self.dtype:
+            raise TypeError(f"a tensor of {self.dtype} expected, not {x.dtype}")
+        if x.device != self._on:
+            raise _elsewhere(x, self._on)
         if other is not None:
             if other.shape != x.shape or other.dtype != x.dtype:
                 raise ValueError(f"tensors of one shape and type expected, not {(m, c)} and {tuple(other.shape)}")
-            _require_device(other, self.y)
+            if other.device != self._on:
+                raise _elsewhere(other, self._on)
         return m
 
     def _param(self, p: torch.Tensor) -> int:
         if p.shape != (self.C,) or p.dtype != torch.float32 or not p.is_contiguous():
             raise ValueError(f"gamma and beta are fp32 vectors of {self.C}")
-        _require_device(p, self.y)
+        if p.device != self._on:
+            raise _elsewhere(p, self._on)
         return p.data_ptr()
 
     def forward(self, x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor | None = None,
@@ -342,7 +353,8 @@ class Norm8:
         """dx (with dsum, the gradient that reaches the sum another way, added), dgamma and dbeta
         (None for the root-mean-square norm), of as many rows as the last forward kept."""
         m = self._check(dy, dsum)
-        _require_kept(m, self._rows)
+        if m != self._rows:
+            raise _not_kept(m, self._rows)
         ds = (0, 0) if dsum is None else (dsum.data_ptr(), N._ld(dsum))
         N._check(self._lib.shiftquant_norm8_backward(
             dy.data_ptr(), self._dtype, m, self.C, N._ld(dy), *self._backward, self._param(gamma), *ds, *self._grads,
