@@ -10,8 +10,10 @@
 // Streaming passes, bound by HBM: a thread takes eight consecutive elements (16-byte loads of
 // 16-bit types, 8-byte stores of codes), four threads a scale block.  Where rows are not 16-byte
 // aligned the accesses are an element per lane, and change hands in shared memory.  Measured at 16384 x 11008
-// bf16: gated SiLU forward 236 us (6.2 TB/s), backward 223 us (6.5); GELU 202 us (4.5) and 184 us (4.9), bound
-// by issue; fp32 GELU of 5003 x 1155, unaligned, 20 us either way.
+// bf16: gated SiLU forward 236 us (6.2 TB/s), backward 231 us (6.4); SiLU 173 and 168 us (5.3 and 5.4); tanh
+// GELU 178 and 174; GELU 208 and 195 us (4.4 and 4.7 TB/s), where no unit is full: issue slots 67% and 61%
+// busy, DRAM 48% and 55%, at 44% and 32% of the warps an SM holds.  fp32 GELU of 5003 x 1155, unaligned,
+// 21 us either way.
 #include <cuda_runtime.h>
 
 #include <cstring>
@@ -57,7 +59,7 @@ __device__ constexpr float kTail16[6] = {0.1201210618019104f,    0.1131270229816
 // within 10 units of 2^-24 of itself).  x^2 is kept in two parts, so that its rounding does not
 // grow into the exponential; 2^f on [-1/2, 1/2] and the tail's factor tail / (t exp(-x^2 / 2)),
 // t = 1 / (1 + 0.35 |x|), are polynomials of least relative error fitted on Chebyshev nodes in 64 bits
-// (to 4e-9, and 3.2e-8 over |x| < 14.5).  CUDA's normcdff and expf took 157 instructions an element here.
+// (with their FP32 coefficients within 1.6e-8, and 5.9e-8 over |x| < 14.5).  CUDA's normcdff and expf took 157 instructions an element here.
 __device__ __forceinline__ void normal_tail(float x, float& tail, float& g) {
   float y;
   asm("{\n\t.reg .f32 a;\n\tabs.f32 a, %1;\n\tmin.NaN.f32 %0, a, 0f41800000;\n\t}" : "=f"(y) : "f"(x));   // at most 16

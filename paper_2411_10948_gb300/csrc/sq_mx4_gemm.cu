@@ -510,7 +510,9 @@ struct Mx4Rows {
   const void* x;
   int64_t ld, K;
   int vec;
-  int by_warp;   // at most four rows: a stage is one warp's, and the warps take the stages in turn
+  // at most four rows: a stage is one warp's (eight blocks of each row), and the warps take the stages in turn.
+  // One row through 4096 x 11008 7.5 us, 10.0 where all four warps share each stage; 4096 x 4096 5.0 and 5.2
+  int by_warp;
 };
 
 // A block of 32 elements of a row on its way to a thread.
@@ -816,7 +818,12 @@ static int launch_pair(Mx4Gemm& g, const Mx4Operand& a, const Mx4Operand& b, int
   return launch_clusters(mx4_pair_kernel<T>, dim3(2 * pairs), kPThreads, kPSmem, 2, s, "mx4_pair_kernel launch", g);
 }
 
-constexpr int kQuantRows = 32;   // rows that a product quantizes itself
+// Rows that a product quantizes itself: what one scale operand's first 32 rows hold, for callers without room
+// for their codes.  Against the quantizer and the product as two launches (us a call, graphs, weights from
+// HBM): 1 row through 4096 x 11008 7.5 for 9.1, 4096 x 4096 5.0 for 7.1; 5 rows 10.9 for 9.4 and 5.9 for 7.7,
+// 16 rows 11.4 for 9.6 and 6.3 for 8.0, 32 rows 15.3 for 10.0 and 7.9 for 8.4, 17 rows through 1155 x 1001
+// 12.6 for 7.1: one launch is the faster one up to four rows, and further on for some weights alone.
+constexpr int kQuantRows = 32;
 // whether a product takes the form of few rows: its column tiles are the grid's y
 static bool few_rows(int64_t M, int64_t N) { return M <= kQuantRows && (N + 127) / 128 <= 65535; }
 
@@ -850,6 +857,10 @@ static int run_mx4(Mx4Gemm& g, const Mx4Operand& a, const Mx4Operand& b, int64_t
     if (g.M <= 16) return launch_split<T, 16, false>(g, a, nullptr, b, K, dev, sms, s);
     return launch_split<T, 32, false>(g, a, nullptr, b, K, dev, sms, s);
   }
+  // CTA pairs from a quarter of the SMs in tiles on.  Pairs and split, us (bf16 out): M x K x N = 1536 x 4096 x 1792 (42
+  // tiles) 9.4 and 11.6, 2048 x 11008 x 1280 16.6 and 22.2, 256 x 4096 x 11008 10.3 and 12.4, but 33 x 4096 x
+  // 11008 10.6 and 9.4; below, 512 x 4096 x 512 8.4 and 6.9, 128 x 11008 x 4096 16.2 and 12.9, but 1024 x 1024 x 1024
+  // (16 tiles) 5.6 and 8.6, 1536 x 4096 x 1536 9.1 and 11.0: the best threshold falls with K
   const int64_t tiles = ((g.M + 255) / 256) * ((g.N + 255) / 256);
   if (tiles >= sms / 4) return launch_pair<T>(g, a, b, K, dev, sms, s);
   // 128 rows where their blocks, each with a K range of a stage at least, fill the SMs, else 64.  No fewer

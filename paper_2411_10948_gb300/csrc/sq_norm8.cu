@@ -129,7 +129,10 @@ __device__ __forceinline__ float2 row_sum(float2 v, RowRed<kTwo>& all, int& half
 // 7.0 TB/s; 100000 x 768 bf16 layer norm 113 us, 6.1 TB/s), by the latency of a block's life where rows are
 // fewer (12608 x 768 20.5 us, 4.3 TB/s).  Sums, squares and outputs go two elements per instruction, and the
 // rounded sum is stored as it is read back: element by element these took 92, 148 and 25 us.  (One wave of blocks that walk the rows, the next row on its way: 64 registers spill, more
-// leave too few warps; 16384 x 4096 bf16 99 us.)
+// leave too few warps; 16384 x 4096 bf16 99 us.)  Three blocks per SM are asked for in 16-bit RMS norms of
+// two chunks a thread: 16384 x 8192 bf16 181 us for 202, x 4096 89 for 90; layer norms take the same time
+// with a bound and without.  Beyond 16384 columns: 4096 x 20000 bf16 RMS with a residual 154 us, fp32
+// layer 256 us (4.8 and 5.4 TB/s of what they have to move).
 template <typename T, int kChunks, bool kVec, bool kBlock, bool kLayer>
 __global__ void __launch_bounds__(512, kVec && kBlock && kChunks == 2 && sizeof(T) == 2 && !kLayer ? 3 : 1) norm8_forward_kernel(const Norm8Args a) {
   __shared__ RowRed<false> red;
@@ -254,7 +257,9 @@ __global__ void __launch_bounds__(512, kVec && kBlock && kChunks == 2 && sizeof(
 // Rows group by group; the column sums of dgamma and dbeta stay in a thread's registers (in its
 // group's row of the workspace for kChunks = 0) until the group's rows are done.  Beyond two chunks the
 // sums leave no room for the row, which is read twice.  Bound by the instructions of element-wise accesses
-// (5003 x 1155 fp32 35 us for 42 with scalar arithmetic and parameters, 12608 x 767 bf16 48 for 57).
+// (5003 x 1155 fp32 35 us for 42 with scalar arithmetic and parameters, 12608 x 767 bf16 48 for 57); for
+// kChunks = 0 by the column sums' way through the workspace, two reads and writes per element (4096 x 20000 bf16 RMS
+// 864 us, fp32 layer norm 913).
 template <typename T, int kChunks, bool kVec, bool kBlock, bool kLayer>
 __global__ void __launch_bounds__(512) norm8_backward_kernel(const Norm8Args a) {
   __shared__ RowRed<kLayer> red;
